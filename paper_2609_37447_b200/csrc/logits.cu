@@ -571,7 +571,8 @@ __global__ void __launch_bounds__(kThreads, kItems > 4 ? 1 : 1024 / kThreads) lo
             }
             __syncthreads();
             whole = row_part;
-            factor = exp2_approx((base - (whole.top == -INFINITY ? 0.0f : whole.top)) * scale);
+            // (a slice with nothing above -infinity has exponentials of 0 and no max to compare: base is 0 there, far above a low row max)
+            factor = mine.top == -INFINITY ? 0.0f : exp2_approx((base - whole.top) * scale);
         }
         const bool empty = whole.top == -INFINITY;
         if (rank == 0 && tid == 0) {

@@ -1,0 +1,68 @@
+"""The token calls (include/az_tokens.h) at the ends of what they allow: slices of a row that hold nothing, scales and sizes near
+the limits of their types.  Statements in 64 bits and tolerances as in test_gpu_tokens.py."""
+import math
+
+import pytest
+import torch
+
+from test_gpu_tokens import BF16, F32, TYPES, U, az, clean_status, gen, half_step, smallest  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+# ---- logits: CTAs of a cluster whose share of the row holds nothing ------------------------------------------
+
+# what the few tokens that are left have for logits, and the temperature
+LOW_ROWS = [(-1.0, 0.01), (-5.0, 0.05), (-10.0, 0.05), (-9.0, 0.1), (-45.0, 0.5), (-100.0, 1.0), (-200.0, 1.0), (30.0, 0.02), (-0.01, 1.0)]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("vocab", [1858, 5000, 40000, 100277, 131072, 200003])
+@pytest.mark.parametrize("closed_by", ["mask", "logits", "both", "lowest"])
+@pytest.mark.parametrize("tokens", [1, 3])
+def test_low_logits_beside_slices_that_hold_nothing(az, dtype, vocab, closed_by, tokens):
+    """A strict grammar at a low temperature: a few tokens with low logits, nothing in most CTAs' shares of the row."""
+    rows = len(LOW_ROWS)
+    level, heat = (torch.tensor(v, device="cuda", dtype=F32) for v in zip(*LOW_ROWS))
+    place = torch.tensor([vocab // 3, vocab // 3 + 1, vocab - 1][:tokens], device="cuda")
+    spread = torch.tensor([0.0, -0.5, -1.0][:tokens], device="cuda")
+    kept = (level[:, None] + spread * heat[:, None]).to(dtype)
+    closed = {"mask": 0.5, "lowest": torch.finfo(dtype).min}.get(closed_by, -math.inf)
+    logits = torch.full((rows, vocab), closed, device="cuda", dtype=dtype)
+    logits[:, place] = kept
+    rules = {"temperature": heat}
+    if closed_by in ("mask", "both"):
+        bits = torch.zeros(-(-vocab // 32) * 32, dtype=torch.int64, device="cuda")
+        bits[place] = 1
+        words = (bits.view(-1, 32) << torch.arange(32, device="cuda")).sum(1)
+        rules["allowed"] = torch.where(words >= 2 ** 31, words - 2 ** 32, words).int()
+    x = (kept.double() - kept.double().amax(1, keepdim=True)) / heat.double()[:, None]
+    total = x.exp().sum(1, keepdim=True)
+    want = x.exp() / total
+    rel = (12 * kept.double().abs().amax(1, keepdim=True) / heat.double()[:, None] + 5 * x.abs() + 120) * U
+    rest = torch.ones(vocab, dtype=torch.bool, device="cuda")
+    rest[place] = False
+    for kind in {dtype, F32}:
+        probs = torch.full((rows, vocab), -1.0, device="cuda", dtype=kind)
+        best = torch.empty(rows, dtype=torch.int32, device="cuda")
+        logprob = torch.empty(rows, device="cuda")
+        az.az_token_probs(logits, probs, best, logprob, **rules)
+        assert (probs[:, rest] == 0).all()
+        assert ((probs[:, place].double() - want).abs() <= (rel + half_step(kind)) * want + smallest(kind)).all()
+        top = kept.double().argmax(1)
+        assert torch.equal(best.long(), place[top])
+        assert ((logprob.double() + total.log()[:, 0]).abs() <= 2 * rel.amax(1) + 1e-7).all()
+
+
+def test_every_slice_but_one_holds_nothing_wherever_it_is(az):
+    """One token left, in each chunk of the row in turn."""
+    vocab, rows = 131072, 512
+    place = torch.arange(rows, device="cuda") * 256 + 17
+    logits = torch.full((rows, vocab), -math.inf, device="cuda", dtype=BF16)
+    logits[torch.arange(rows, device="cuda"), place] = -300.0
+    probs = torch.empty_like(logits)
+    best = torch.empty(rows, dtype=torch.int32, device="cuda")
+    logprob = torch.empty(rows, device="cuda")
+    az.az_token_probs(logits, probs, best, logprob)
+    assert torch.equal(best.long(), place) and (logprob == 0).all()
+    assert (probs != 0).sum() == rows and (probs[torch.arange(rows, device="cuda"), place] == 1).all()
