@@ -352,6 +352,7 @@ block_matmul_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
                 }
         } else if (warp == 1) {
             // ---- issuer: four K = 32 steps per block, the first of which overwrites the slot
+            // (barriers that threads of the pair's other CTA arrive on are waited for with acquire at cluster scope)
             const uint32_t idesc = ptx::idesc_e4m3_f32(kRows, kTurned ? args.a_rows : kSlotCols);
             // 128-byte swizzle (2 at bit 61), 8-row groups 1024 bytes apart, descriptor version 1
             constexpr uint32_t desc_hi = (1024u >> 4) | (1u << 14) | (2u << 29);
@@ -362,12 +363,12 @@ block_matmul_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
     #pragma unroll 1
             for (int c = c_begin; c < c_end; ++c) {
                     ok = bounded_wait(bar_full(s), phase, abort_flag, &g_status, kStatusWaitTimeout, kSpinLimit);
-                    if (kPair) ok = ok && bounded_wait(bar_peer(s), phase, abort_flag, &g_status, kStatusWaitTimeout, kSpinLimit);
+                    if (kPair) ok = ok && bounded_wait<true>(bar_peer(s), phase, abort_flag, &g_status, kStatusWaitTimeout, kSpinLimit);
                     const uint32_t at = tiles_at + (uint32_t)s * stage_bytes;
                     const uint32_t a_lo = ((at >> 4) & 0x3fffu) | (1u << 16), b_lo = (((at + a_bytes) >> 4) & 0x3fffu) | (1u << 16);
 #pragma unroll
                     for (int h = 0; h < kSlotsPerBlock; ++h) {
-                        ok = ok && bounded_wait(bar_free(t), t_phase ^ 1u, abort_flag, &g_status, kStatusWaitTimeout, kSpinLimit);
+                        ok = ok && bounded_wait<kPair>(bar_free(t), t_phase ^ 1u, abort_flag, &g_status, kStatusWaitTimeout, kSpinLimit);
                         if (!ok) break;
                         ptx::tc_fence_after();
                         const uint32_t b_half = b_lo + (uint32_t)(h * (kTileM / kSlotsPerBlock) * kBlockK >> 4);

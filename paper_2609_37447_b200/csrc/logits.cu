@@ -555,10 +555,10 @@ __global__ void __launch_bounds__(kThreads, kItems > 4 ? 1 : 1024 / kThreads) lo
                 ptx::st_async_cluster_v4(ptx::map_to_cta(ptx::smem_addr(&parts[turn][rank]), (uint32_t)tid), __float_as_uint(mine.top), (uint32_t)mine.index,
                                          __float_as_uint(mine.sum), 0u, ptx::map_to_cta(ptx::smem_addr(&arrived[turn]), (uint32_t)tid));
             }
-            // the first warp waits for all of them and tells the others.  (A wait that runs out, which none does short of a fault,
-            // leaves the row with what has come in.)
+            // the first warp waits for all of them (acquire at cluster scope: other CTAs wrote them) and tells the others.  (A wait that
+            // runs out, which none does short of a fault, leaves the row with what has come in.)
             if (warp == 0) {
-                bounded_wait(ptx::smem_addr(&arrived[turn]), phase, &abort_flag, &g_status, kStatusWaitTimeout, 1u << 24);
+                bounded_wait<true>(ptx::smem_addr(&arrived[turn]), phase, &abort_flag, &g_status, kStatusWaitTimeout, 1u << 24);
                 Part p = {-INFINITY, 0x7fffffff, 0.0f, 0u};
                 if (lane < cluster) p = parts[turn][lane];     // (a lane per CTA)
                 whole.top = warp_max_nan(p.top);
