@@ -355,14 +355,15 @@ __global__ void __launch_bounds__(kThreads, kItems > 4 ? 1 : 1024 / kThreads) lo
         rest(max(kTokens * kThreads, prompt), said, false);
     }
     // ---- biases: is a token of the slice listed twice
+    // (entries are unsigned: a list may end at 2^31 - 1, and the steps beyond its end leave 31 bits)
     int bias_slot = -1;                                        // this thread's first entry
     float bias_value = 0.0f;
     bool twice = false;
-    if (begin + tid < stop) {
+    if (tid < stop - begin) {
         bias_slot = slot(next_bias_tokens[tid]);
         bias_value = next_bias_values[tid];
         twice = bias_slot >= 0 && touch(claimed, bias_slot);
-        for (int e = begin + tid + kThreads; e < stop; e += kThreads) {
+        for (uint32_t e = (uint32_t)begin + tid + kThreads; e < (uint32_t)stop; e += kThreads) {
             const int s = slot(a.r.bias_tokens[e]);
             if (s >= 0 && touch(claimed, s)) twice = true;
         }
@@ -406,14 +407,14 @@ __global__ void __launch_bounds__(kThreads, kItems > 4 ? 1 : 1024 / kThreads) lo
         };
         if (!any_twice) {
             if (bias_slot >= 0) add(bias_slot, bias_value);
-            for (int e = begin + tid + kThreads; e < stop; e += kThreads) {
+            for (uint32_t e = (uint32_t)begin + tid + kThreads; e < (uint32_t)stop; e += kThreads) {
                 const int s = slot(a.r.bias_tokens[e]);
                 if (s >= 0) add(s, a.r.bias_values[e]);
             }
         } else if (warp == 0) {
-            for (int e0 = begin; e0 < stop; e0 += 32) {
-                const int e = e0 + lane;
-                const int s = e < stop ? slot(a.r.bias_tokens[e]) : -1;
+            for (uint32_t e0 = (uint32_t)begin; e0 < (uint32_t)stop; e0 += 32) {
+                const uint32_t e = e0 + lane;
+                const int s = e < (uint32_t)stop ? slot(a.r.bias_tokens[e]) : -1;
                 const float b = s >= 0 ? a.r.bias_values[e] : 0.0f;
                 const uint32_t same = __match_any_sync(0xffffffffu, s);
                 const bool leader = s >= 0 && lane == __ffs(same) - 1;

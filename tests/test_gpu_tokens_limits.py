@@ -66,3 +66,39 @@ def test_every_slice_but_one_holds_nothing_wherever_it_is(az):
     az.az_token_probs(logits, probs, best, logprob)
     assert torch.equal(best.long(), place) and (logprob == 0).all()
     assert (probs != 0).sum() == rows and (probs[torch.arange(rows, device="cuda"), place] == 1).all()
+
+
+# ---- indices near 2^31 ---------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("twice", [False, True])
+def test_bias_lists_that_end_at_the_last_index(az, twice):
+    """Lists at the end of 2^31 - 1 entries give what the same lists give in a short buffer."""
+    count = 2 ** 31 - 1
+    lengths = [600, 0, 700, 1, 31]
+    total = sum(lengths)
+    short = torch.tensor([0] + lengths, device="cuda").cumsum(0).int()
+    long_tokens = torch.zeros(count, dtype=torch.int32, device="cuda")
+    long_values = torch.full((count,), 100.0, device="cuda")
+    for vocab in (1858, 9000, 131072):
+        g = gen(vocab)
+        tokens = torch.cat([torch.randperm(vocab, generator=g, device="cuda")[:n] for n in lengths]).int()
+        if twice:
+            tokens[5:600:7] = tokens[3]
+            tokens[total - 1] = tokens[total - 2]
+        values = torch.randn(total, generator=g, device="cuda")
+        long_tokens[count - total:] = tokens
+        long_values[count - total:] = values
+        logits = torch.randn(len(lengths), vocab, generator=g, device="cuda")
+        want, got = torch.empty_like(logits), torch.empty_like(logits)
+        az.az_adjust_logits(logits, want, bias_offsets=short, bias_tokens=tokens, bias_values=values)
+        az.az_adjust_logits(logits, got, bias_offsets=short + (count - total), bias_tokens=long_tokens, bias_values=long_values)
+        assert torch.equal(want, got)
+        exact = logits.double()
+        if not twice:
+            owner = torch.repeat_interleave(torch.arange(len(lengths), device="cuda"), torch.tensor(lengths, device="cuda"))
+            exact = exact.index_put((owner, tokens.long()), values.double(), accumulate=True)
+            assert ((got.double() - exact).abs() <= U * exact.abs()).all()
+    # offsets beyond the buffer are clamped to it: lists that hold nothing
+    none = torch.full((len(lengths) + 1,), 2 ** 31 - 1, dtype=torch.int32, device="cuda")
+    az.az_adjust_logits(logits, got, bias_offsets=none, bias_tokens=long_tokens, bias_values=long_values)
+    assert torch.equal(got, logits)
