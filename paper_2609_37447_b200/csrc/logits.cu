@@ -186,7 +186,7 @@ __global__ void __launch_bounds__(kThreads, kItems > 4 ? 1 : 1024 / kThreads) lo
     // does the row fill the groups number i of the whole CTA
     auto inner_item = [&](int i, int head, int end) { return chunk_at(i * kWarps) >= head && chunk_at(i * kWarps + kWarps - 1) + kChunk <= end; };
     // a row on its way into this thread's own places: whole groups by asynchronous copies, the ends one by one
-    auto fetch = [&](int row, int into, int begin, int stop) {
+    auto fetch = [&](uint32_t row, int into, int begin, int stop) {
         const T *in_row = static_cast<const T *>(a.logits) + row * a.logits_stride;
         const int head = head_of(in_row), end = a.vocab + head;
         auto copy = [&](int i, int v) {
@@ -230,7 +230,7 @@ __global__ void __launch_bounds__(kThreads, kItems > 4 ? 1 : 1024 / kThreads) lo
         }
     };
     // a row's part of the bias lists: as the offsets say it, and made fit
-    auto biases_of = [&](int row, int &begin, int &stop) {
+    auto biases_of = [&](uint32_t row, int &begin, int &stop) {
         if (biased) { begin = a.r.bias_offsets[row]; stop = a.r.bias_offsets[row + 1]; }
     };
     auto clamp_biases = [&](int &begin, int &stop) {
@@ -238,8 +238,8 @@ __global__ void __launch_bounds__(kThreads, kItems > 4 ? 1 : 1024 / kThreads) lo
         begin = min(max(begin, 0), (int)a.r.bias_count);
         stop = min(max(stop, begin), (int)a.r.bias_count);
     };
-    const int row_step = (int)(gridDim.x / cluster);
-    int row = (int)(blockIdx.x / cluster);
+    const uint32_t rows = (uint32_t)a.rows, row_step = gridDim.x / (uint32_t)cluster;
+    uint32_t row = blockIdx.x / (uint32_t)cluster;             // (unsigned: a step beyond the last of 2^31 - 1 rows leaves 31 bits)
     int turn = 0;
     uint32_t phase = 0;                                       // of arrived[]: of both, it flips after two rows
     int begin = 0, stop = 0, next_begin = 0, next_stop = 0;
@@ -250,7 +250,7 @@ __global__ void __launch_bounds__(kThreads, kItems > 4 ? 1 : 1024 / kThreads) lo
     if (cluster > 1) ptx::cluster_wait();
     __syncthreads();                                          // words and bits are clear
 
-    for (; row < a.rows; row += row_step, phase ^= (uint32_t)turn, turn ^= 1, begin = next_begin, stop = next_stop) {
+    for (; row < rows; row += row_step, phase ^= (uint32_t)turn, turn ^= 1, begin = next_begin, stop = next_stop) {
     if (kProbs && cluster > 1 && tid == 0) ptx::mbar_arrive_expect_tx(ptx::smem_addr(&arrived[turn]), (uint32_t)cluster * sizeof(Part));
     // ---- the row's logits, parameters and mask are in shared memory
     copies_wait();
@@ -263,8 +263,8 @@ __global__ void __launch_bounds__(kThreads, kItems > 4 ? 1 : 1024 / kThreads) lo
     const int said = counting ? min(max((int)param[0], 0), (int)a.r.token_room) : 0;
     const int prompt = counting && a.r.prompt_lengths ? min(max((int)param[1], 0), said) : 0;
     const float temperature = a.r.temperature ? __uint_as_float(param[5]) : 1.0f;
-    const int after = row + row_step;
-    if (after < a.rows) biases_of(after, next_begin, next_stop);
+    const uint32_t after = row + row_step;
+    if (after < rows) biases_of(after, next_begin, next_stop);
     // what is allowed, where something may not be: a byte per group (bit j: element j is inside the row and its mask)
     bool inner = true;
 #pragma unroll
@@ -460,7 +460,7 @@ __global__ void __launch_bounds__(kThreads, kItems > 4 ? 1 : 1024 / kThreads) lo
             }
         }
     }
-    if (after < a.rows) {
+    if (after < rows) {
         clamp_biases(next_begin, next_stop);                   // (only now: the offsets are on their way until here)
         fetch(after, turn ^ 1, next_begin, next_stop);
     }

@@ -102,3 +102,23 @@ def test_bias_lists_that_end_at_the_last_index(az, twice):
     none = torch.full((len(lengths) + 1,), 2 ** 31 - 1, dtype=torch.int32, device="cuda")
     az.az_adjust_logits(logits, got, bias_offsets=none, bias_tokens=long_tokens, bias_values=long_values)
     assert torch.equal(got, logits)
+
+
+def test_the_largest_number_of_rows(az):
+    """2^31 - 1 rows of one token: the step behind the last row leaves 31 bits, and nothing in front of the buffers is touched."""
+    rows, guard = 2 ** 31 - 1, 1 << 20
+    flat = torch.full((guard + rows + guard,), 3.0, device="cuda", dtype=BF16)
+    logits = flat[guard:guard + rows].view(rows, 1)
+    nothing, all_of_it = (torch.full((1,), v, dtype=torch.int32, device="cuda") for v in (0, -1))
+    best = torch.full((rows,), -7, dtype=torch.int32, device="cuda")
+    logits[::5] = -math.inf
+    az.az_token_probs(logits, best=best, allowed=all_of_it)
+    assert (best[::5] == -1).all()
+    best[::5] = 0
+    assert (best == 0).all()
+    az.az_adjust_logits(logits, logits, allowed=nothing)
+    assert (flat[guard:guard + rows] == -math.inf).all()
+    assert (flat[:guard] == 3.0).all() and (flat[guard + rows:] == 3.0).all()
+    az.az_token_probs(logits, logits, best)                   # rows that hold nothing, in place
+    assert (flat[guard:guard + rows] == 0).all() and (best == -1).all()
+    assert (flat[:guard] == 3.0).all() and (flat[guard + rows:] == 3.0).all()
