@@ -133,9 +133,20 @@ int az_token_probs(const void *logits_dev, int type, int rows, int vocab, int64_
                    void *probs_dev, int probs_type, int64_t probs_stride, int32_t *best_dev, float *best_logprob_dev,
                    void *cuda_stream);
 
-/* Status word of the current device's calls of this header so far (0 = clean; it is cleared).  Synchronises the given
- * stream.  AZ_ERR_DEVICE_TIMEOUT if a bounded wait ran out: outputs of the calls since the last read are then incomplete. */
+/*
+ * Status word of the current device's calls of this header (0 = clean).  Synchronises the given stream, so calls queued there or
+ * finished elsewhere are covered; what a call still running on another stream raises is left for a later read.  The bits that are
+ * returned are cleared, others are not touched.  AZ_ERR_DEVICE_TIMEOUT if a bounded wait ran out: outputs of the calls since the
+ * last read are then incomplete.
+ */
 int az_tokens_status(void *cuda_stream, uint32_t *status_out);
+
+/*
+ * Self-test of that report: queues a one-CTA kernel whose wait runs out (after a millisecond) and raises the status bit, as a
+ * wait would in the product's kernels (part 0) or in the logit calls' (part 1).  The next az_tokens_status returns
+ * AZ_ERR_DEVICE_TIMEOUT, the one after it is clean.  Nothing hangs or traps.  Errors: BAD_ARG (part), CUDA.
+ */
+int az_selftest_tokens_timeout(int part, void *cuda_stream);
 
 #ifdef __cplusplus
 }

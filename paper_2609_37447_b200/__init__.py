@@ -29,7 +29,7 @@ EXPORTS = ("az_position_bytes", "az_policy_size", "az_mask_words", "az_value_siz
            "az_last_cuda_error",
            "az_apply_moves", "az_standin_evaluate", "az_search_create", "az_search_destroy", "az_search_set_roots", "az_search_replace_roots",
            "az_search_run", "az_search_run_async", "az_search_wait", "az_search_root", "az_search_root_visits", "az_search_advance", "az_search_root_noise", "az_search_root_positions", "az_search_tree", "az_search_launches_per_step",
-           "az_quantise_blocks", "az_block_matmul", "az_adjust_logits", "az_token_probs", "az_tokens_status")
+           "az_quantise_blocks", "az_block_matmul", "az_adjust_logits", "az_token_probs", "az_tokens_status", "az_selftest_tokens_timeout")
 
 
 class az_arch(ctypes.Structure):
@@ -169,6 +169,8 @@ def _load_library():
     lib.az_token_probs.argtypes = [vp, ci, ci, ci, i64, rp, vp, ci, i64, vp, vp, vp]
     lib.az_tokens_status.restype = ci
     lib.az_tokens_status.argtypes = [vp, ctypes.POINTER(ctypes.c_uint32)]
+    lib.az_selftest_tokens_timeout.restype = ci
+    lib.az_selftest_tokens_timeout.argtypes = [ci, vp]
     return lib
 
 
@@ -605,9 +607,15 @@ def az_token_probs(logits, probs=None, best=None, best_logprob=None, tokens=None
 
 
 def az_tokens_status(stream=None) -> int:
-    """Status word of the current device's calls of the four above since the last read (0 = clean)."""
+    """Status word of the current device's calls of the four above (0 = clean); what it returns is cleared.  Synchronises the stream
+    only: calls that still run on other streams are left for a later read."""
     word = ctypes.c_uint32(0)
     code = _lib.az_tokens_status(_stream_ptr(stream), ctypes.byref(word))
     if code not in (AZ_OK, AZ_ERR_DEVICE_TIMEOUT):
         raise AzError(code, "az_tokens_status")
     return int(word.value)
+
+
+def az_selftest_tokens_timeout(part, stream=None):
+    """Queues a wait that runs out, of the product's (part 0) or the logit calls' (part 1): the next az_tokens_status reports it."""
+    _check(_lib.az_selftest_tokens_timeout(part, _stream_ptr(stream)), "az_selftest_tokens_timeout")

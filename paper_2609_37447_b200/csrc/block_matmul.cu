@@ -773,6 +773,17 @@ int launch(const void *a, int64_t a_stride, const void *b, int64_t b_stride, int
                                          : launch_form<kFew, 2>(map_a, map_b, args, grid, smem, dev, s);
 }
 
+// the status words of the calls of az_tokens.h on the current device: the product's, the logit calls'
+int status_words(uint32_t *(&words)[2]) {
+    AZ_CUDA(cudaGetSymbolAddress(reinterpret_cast<void **>(&words[0]), g_status));
+    return logits_status_word(&words[1]);
+}
+
+__global__ void clear_bits_kernel(uint32_t *a, uint32_t a_bits, uint32_t *b, uint32_t b_bits) {
+    atomicAnd(a, ~a_bits);
+    atomicAnd(b, ~b_bits);
+}
+
 }  // namespace
 }  // namespace az
 
@@ -806,14 +817,23 @@ extern "C" int az_block_matmul(const void *a_dev, int64_t a_stride, const float 
 extern "C" int az_tokens_status(void *cuda_stream, uint32_t *status_out) {
     if (!status_out) return AZ_ERR_BAD_ARG;
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-    void *word = nullptr;
-    AZ_CUDA(cudaGetSymbolAddress(&word, az::g_status));
-    AZ_CUDA(cudaMemcpyAsync(status_out, word, sizeof(uint32_t), cudaMemcpyDeviceToHost, s));
-    AZ_CUDA(cudaMemsetAsync(word, 0, sizeof(uint32_t), s));
-    uint32_t logits = 0;
-    const int rc = az::logits_status(s, &logits);
+    uint32_t *words[2] = {}, seen[2] = {0, 0};
+    const int rc = az::status_words(words);
     if (rc != AZ_OK) return rc;
+    for (int i = 0; i < 2; ++i) AZ_CUDA(cudaMemcpyAsync(&seen[i], words[i], sizeof(uint32_t), cudaMemcpyDeviceToHost, s));
     AZ_CUDA(cudaStreamSynchronize(s));
-    *status_out |= logits;
+    *status_out = seen[0] | seen[1];
+    if (*status_out == 0) return AZ_OK;
+    // what this call reports is cleared, bit by bit, and nothing else: kernels on other streams may raise a bit at any time
+    az::clear_bits_kernel<<<1, 1, 0, s>>>(words[0], seen[0], words[1], seen[1]);
+    AZ_CUDA(cudaGetLastError());
+    AZ_CUDA(cudaStreamSynchronize(s));
     return (*status_out & az::kStatusWaitTimeout) ? AZ_ERR_DEVICE_TIMEOUT : AZ_OK;
+}
+
+extern "C" int az_selftest_tokens_timeout(int part, void *cuda_stream) {
+    if (part < 0 || part > 1) return AZ_ERR_BAD_ARG;
+    uint32_t *words[2] = {};
+    const int rc = az::status_words(words);
+    return rc == AZ_OK ? az::raise_wait_timeout(words[part], static_cast<cudaStream_t>(cuda_stream)) : rc;
 }

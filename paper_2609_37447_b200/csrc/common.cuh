@@ -229,7 +229,9 @@ size_t fc_tc_weight_bytes(int n, bool policy);
 void fc_tc_pack_weights(const float *w, int n, bool policy, __nv_bfloat16 *packed);     // w[n][32*64], K permuted to square*32 + channel; policy: the tile height of the head GEMM's CTA pairs
 int launch_fc_tc(const Net &net, int batch, float *value_out, cudaStream_t s);
 
-// device-side status of the logit calls (logits.cu), read and cleared on the stream
-int logits_status(cudaStream_t s, uint32_t *out);
+// the current device's status word of the logit calls (logits.cu)
+int logits_status_word(uint32_t **word);
+// a kernel whose wait runs out and says so in the word (selftest.cu)
+int raise_wait_timeout(uint32_t *status, cudaStream_t s);
 
 }  // namespace az

@@ -723,11 +723,8 @@ int launch_type(const Args &a, int type, int rows, cudaStream_t s) {
 
 }  // namespace
 
-int logits_status(cudaStream_t s, uint32_t *out) {
-    void *word = nullptr;
-    AZ_CUDA(cudaGetSymbolAddress(&word, g_status));
-    AZ_CUDA(cudaMemcpyAsync(out, word, sizeof(uint32_t), cudaMemcpyDeviceToHost, s));
-    AZ_CUDA(cudaMemsetAsync(word, 0, sizeof(uint32_t), s));
+int logits_status_word(uint32_t **word) {
+    AZ_CUDA(cudaGetSymbolAddress(reinterpret_cast<void **>(word), g_status));
     return AZ_OK;
 }
 }  // namespace az

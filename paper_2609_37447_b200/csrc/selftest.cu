@@ -1,6 +1,7 @@
-// az_selftest_wait_timeout: exercises the bounded-wait path that every mbarrier wait of the
-// tensor-core kernels goes through, without hanging anything: one warp waits on a barrier that
-// nobody will ever arrive on, with a short poll limit, and must come back with the time-out status.
+// az_selftest_wait_timeout, az_selftest_tokens_timeout: exercise the bounded-wait path that every
+// mbarrier wait of the tensor-core and logit kernels goes through, without hanging anything: one warp
+// waits on a barrier that nobody will ever arrive on, with a short poll limit, and must come back with
+// the time-out status.
 #include "common.cuh"
 #include "ptx.cuh"
 
@@ -25,10 +26,16 @@ __global__ void __launch_bounds__(64, 1) wait_timeout_kernel(uint32_t *status, u
         ok = bounded_wait(ptx::smem_addr(&bar), 0, &abort_flag, status, kStatusWaitTimeout, limit * 4);
     }
     __syncthreads();                                   // the common teardown every role reaches
-    if (threadIdx.x == 0) *reached_teardown = ok ? 2 : 1;
+    if (threadIdx.x == 0 && reached_teardown) *reached_teardown = ok ? 2 : 1;
 }
 
 }  // namespace
+
+int raise_wait_timeout(uint32_t *status, cudaStream_t s) {
+    wait_timeout_kernel<<<1, 64, 0, s>>>(status, 1u << 8, nullptr);       // (a poll that finds nothing takes about 4 us)
+    AZ_CUDA(cudaGetLastError());
+    return AZ_OK;
+}
 }  // namespace az
 
 extern "C" int az_selftest_wait_timeout(void *cuda_stream) {

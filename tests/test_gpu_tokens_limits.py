@@ -1,6 +1,9 @@
 """The token calls (include/az_tokens.h) at the ends of what they allow: slices of a row that hold nothing, scales and sizes near
 the limits of their types.  Statements in 64 bits and tolerances as in test_gpu_tokens.py."""
+import ctypes
 import math
+import threading
+import time
 
 import pytest
 import torch
@@ -122,3 +125,53 @@ def test_the_largest_number_of_rows(az):
     az.az_token_probs(logits, logits, best)                   # rows that hold nothing, in place
     assert (flat[guard:guard + rows] == 0).all() and (best == -1).all()
     assert (flat[:guard] == 3.0).all() and (flat[guard + rows:] == 3.0).all()
+
+
+# ---- the status word ------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("part", [0, 1])
+def test_a_wait_that_runs_out_is_reported_once(az, part):
+    az.az_selftest_tokens_timeout(part)
+    word = az.az_tokens_status()
+    assert word != 0 and az.az_tokens_status() == 0
+    raw = ctypes.c_uint32(0)
+    az.az_selftest_tokens_timeout(part)
+    stream = torch.cuda.current_stream().cuda_stream
+    assert az._lib.az_tokens_status(stream, ctypes.byref(raw)) == az.AZ_ERR_DEVICE_TIMEOUT and raw.value == word
+    assert az._lib.az_tokens_status(stream, ctypes.byref(raw)) == az.AZ_OK and raw.value == 0
+    x, y = torch.ones(3, 5000, device="cuda"), torch.empty(3, 5000, device="cuda")
+    az.az_token_probs(x, y)                                   # the device still works
+    assert ((y.double() - 1 / 5000).abs() <= 120 * U / 5000).all()
+
+
+@pytest.mark.parametrize("part", [0, 1])
+def test_no_report_is_lost_between_streams(az, part):
+    """One thread reads the status without a pause while kernels on another stream raise it: every one of them is reported."""
+    reading, raising = torch.cuda.Stream(), torch.cuda.Stream()
+    reports, stop, failed = [0], threading.Event(), []
+
+    def read():
+        try:
+            while not stop.is_set():
+                if az.az_tokens_status(reading):
+                    reports[0] += 1
+        except Exception as e:
+            failed.append(e)
+
+    reader = threading.Thread(target=read)
+    reader.start()
+    try:
+        for i in range(200):
+            before = reports[0]
+            az.az_selftest_tokens_timeout(part, raising)
+            raising.synchronize()
+            limit = time.monotonic() + 5
+            while reports[0] == before and time.monotonic() < limit and not failed:
+                time.sleep(0.0002)
+            assert not failed and reports[0] > before, i
+    finally:
+        stop.set()
+        reader.join()
+    assert az.az_tokens_status() == 0
+    with pytest.raises(az.AzError):
+        az.az_selftest_tokens_timeout(2)
