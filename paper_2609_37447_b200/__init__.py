@@ -2,10 +2,13 @@
 
 Every function has the name and meaning of the C entry point declared in include/az_eval.h; all
 computation happens in the library's CUDA kernels.  PyTorch supplies device memory and streams.
-There is no fallback: if libazeval.so is missing or fails to load, importing raises.
+There is no fallback: if libazeval.so is missing or fails to load, importing raises; if _tokens.so (the
+compiled binding of the token calls) is, the first token call raises.
 """
 import ctypes
+import importlib
 import os
+import threading
 from dataclasses import dataclass
 
 import numpy as np
@@ -175,12 +178,27 @@ def _load_library():
 
 
 _lib = _load_library()
-try:
-    from . import _tokens
-except ImportError as e:
-    raise ImportError(f"{os.path.join(_HERE, '_tokens.so')}: {e}; build it with `python -m paper_2609_37447_b200.build`") from e
-_tokens.connect(*(ctypes.cast(getattr(_lib, name), ctypes.c_void_p).value
-                  for name in ("az_quantise_blocks", "az_block_matmul", "az_adjust_logits", "az_token_probs")))
+
+
+class _TokenCalls:
+    """Stands for the compiled binding of the token calls until the first of them loads it."""
+    _lock = threading.Lock()
+
+    def __getattr__(self, name):
+        global _token_calls
+        with self._lock:
+            if _token_calls is self:
+                try:
+                    binding = importlib.import_module("._tokens", __name__)
+                except ImportError as e:
+                    raise ImportError(f"{os.path.join(_HERE, '_tokens.so')}: {e}; build it with `python -m paper_2609_37447_b200.build`") from e
+                binding.connect(*(ctypes.cast(getattr(_lib, call), ctypes.c_void_p).value
+                                  for call in ("az_quantise_blocks", "az_block_matmul", "az_adjust_logits", "az_token_probs")))
+                _token_calls = binding
+        return getattr(_token_calls, name)
+
+
+_token_calls = _TokenCalls()
 
 
 def _check(code: int, where: str):
@@ -569,7 +587,7 @@ def _stream_arg(stream):
 def az_quantise_blocks(x, codes, scales, block_rows=1, stream=None):
     """x [rows][cols] (float32, bfloat16, float16) -> e4m3 codes [rows][cols] (float8_e4m3fn or uint8) and float32 scales
     [ceil(rows / block_rows)][ceil(cols / 128)]; block_rows 1 (tokens) or 128 (weights)."""
-    code = _tokens.quantise_blocks(x, codes, scales, block_rows, _stream_arg(stream))
+    code = _token_calls.quantise_blocks(x, codes, scales, block_rows, _stream_arg(stream))
     if code:
         raise AzError(code, "az_quantise_blocks")
 
@@ -577,7 +595,7 @@ def az_quantise_blocks(x, codes, scales, block_rows=1, stream=None):
 def az_block_matmul(a, a_scales, b, b_scales, out, bias=None, stream=None):
     """out [m][n] (float32, bfloat16, float16) = a [m][k] times b [n][k] transposed (+ bias [n] float32): e4m3 codes with scales
     [m][ceil(k / 128)] and [ceil(n / 128)][ceil(k / 128)].  Rows of a and b start on 16-byte boundaries."""
-    code = _tokens.block_matmul(a, a_scales, b, b_scales, out, bias, _stream_arg(stream))
+    code = _token_calls.block_matmul(a, a_scales, b, b_scales, out, bias, _stream_arg(stream))
     if code:
         raise AzError(code, "az_block_matmul")
 
@@ -589,7 +607,7 @@ def az_adjust_logits(logits, out, tokens=None, lengths=None, prompt_lengths=None
     tokens [rows][room] int32 with lengths [rows] (and prompt_lengths): the histories; repetition, presence, frequency,
     temperature [rows] float32; bias_offsets [rows + 1], bias_tokens, bias_values: a list per row; allowed: bit masks of int32
     or int64 words, [rows][words] or [words] for all rows (az_legal_masks' as they are)."""
-    code = _tokens.adjust_logits(logits, out, tokens, lengths, prompt_lengths, repetition, presence, frequency,
+    code = _token_calls.adjust_logits(logits, out, tokens, lengths, prompt_lengths, repetition, presence, frequency,
                                  bias_offsets, bias_tokens, bias_values, temperature, allowed, _stream_arg(stream))
     if code:
         raise AzError(code, "az_adjust_logits")
@@ -600,7 +618,7 @@ def az_token_probs(logits, probs=None, best=None, best_logprob=None, tokens=None
                    allowed=None, stream=None):
     """Probabilities [rows][vocab] (float32 or the logits' type), best token [rows] int32 and its log-probability [rows] float32
     under the rules of az_adjust_logits; each output may be left out, not all of them."""
-    code = _tokens.token_probs(logits, probs, best, best_logprob, tokens, lengths, prompt_lengths, repetition, presence, frequency,
+    code = _token_calls.token_probs(logits, probs, best, best_logprob, tokens, lengths, prompt_lengths, repetition, presence, frequency,
                                bias_offsets, bias_tokens, bias_values, temperature, allowed, _stream_arg(stream))
     if code:
         raise AzError(code, "az_token_probs")

@@ -3,7 +3,6 @@ paper_2609_37447_b200/_tokens.so (g++, against the installed torch)."""
 import glob
 import hashlib
 import importlib.metadata
-import importlib.util
 import os
 import subprocess
 import sys
@@ -15,39 +14,56 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libazeval.so")
 BINDING = os.path.join(HERE, "_tokens.so")
 STAMP = os.path.join(HERE, "build", "stamp.txt")
+BINDING_STAMP = os.path.join(HERE, "build", "binding_stamp.txt")
 
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "--expt-relaxed-constexpr"]
 
 
-def _digest() -> str:
-    h = hashlib.sha1(" ".join([*NVCC_FLAGS, importlib.metadata.version("torch"), sys.version]).encode())
-    for path in sorted(glob.glob(os.path.join(CSRC, "*")) + glob.glob(os.path.join(ROOT, "include", "*.h"))):
+def _hash(words, paths) -> str:
+    h = hashlib.sha1(" ".join(words).encode())
+    for path in sorted(paths):
         with open(path, "rb") as f:
             h.update(path.encode() + f.read())
     return h.hexdigest()
 
 
+def _headers() -> list:
+    return glob.glob(os.path.join(ROOT, "include", "*.h"))
+
+
+def _digest() -> str:
+    return _hash(NVCC_FLAGS, glob.glob(os.path.join(CSRC, "*.cu*")) + _headers())
+
+
+def _binding_digest() -> str:
+    return _hash([importlib.metadata.version("torch"), sys.version], [os.path.join(CSRC, "binding.cpp"), *_headers()])
+
+
+def _current(built: str, stamp: str, digest: str) -> bool:
+    return os.path.exists(built) and os.path.exists(stamp) and open(stamp).read().strip() == digest
+
+
 def _binding_command() -> list:
-    torch = os.path.join(importlib.util.find_spec("torch").submodule_search_locations[0])
+    import torch
+    root = os.path.dirname(torch.__file__)
     cuda = os.path.dirname(os.path.dirname(os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")))
-    include = [os.path.join(ROOT, "include"), os.path.join(torch, "include"), os.path.join(torch, "include", "torch", "csrc", "api", "include"),
+    include = [os.path.join(ROOT, "include"), os.path.join(root, "include"), os.path.join(root, "include", "torch", "csrc", "api", "include"),
                os.path.join(cuda, "include"), sysconfig.get_paths()["include"]]
-    return [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", "-D_GLIBCXX_USE_CXX11_ABI=1",
+    return [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden",
+            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}",
             *(f"-I{i}" for i in include), os.path.join(CSRC, "binding.cpp"), "-o", BINDING,
-            "-L" + os.path.join(torch, "lib"), "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10", "-lc10_cuda"]
+            "-L" + os.path.join(root, "lib"), "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10", "-lc10_cuda"]
 
 
-def build(verbose: bool = False, ptxas_info: bool = False) -> str:
-    """Compile every .cu under csrc/ and the binding (in parallel) and link the shared library.  Returns its path."""
+def _build_library(verbose: bool, ptxas_info: bool):
     digest = _digest()
-    if os.path.exists(LIB) and os.path.exists(BINDING) and os.path.exists(STAMP) and open(STAMP).read().strip() == digest and not ptxas_info:
-        return LIB
+    if _current(LIB, STAMP, digest) and not ptxas_info:
+        return
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
-    obj_dir = os.path.join(HERE, "build")
+    obj_dir = os.path.dirname(STAMP)
     os.makedirs(obj_dir, exist_ok=True)
     procs, objs = [], []
-    procs.append(("binding.cpp", subprocess.Popen(_binding_command(), stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
     for src in sorted(glob.glob(os.path.join(CSRC, "*.cu"))):
         obj = os.path.join(obj_dir, os.path.basename(src)[:-3] + ".o")
         objs.append(obj)
@@ -66,6 +82,30 @@ def build(verbose: bool = False, ptxas_info: bool = False) -> str:
     subprocess.run([nvcc, "-shared", "-o", LIB, *objs], check=True)
     with open(STAMP, "w") as f:
         f.write(digest)
+
+
+def _build_binding(verbose: bool):
+    digest = _binding_digest()
+    if _current(BINDING, BINDING_STAMP, digest):
+        return
+    os.makedirs(os.path.dirname(BINDING_STAMP), exist_ok=True)
+    p = subprocess.run(_binding_command(), stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+    if p.returncode != 0 or verbose:
+        sys.stderr.write(f"== binding.cpp\n{p.stdout}\n")
+    if p.returncode != 0:
+        raise RuntimeError(f"{os.environ.get('CXX', 'g++')} failed")
+    with open(BINDING_STAMP, "w") as f:
+        f.write(digest)
+
+
+def build(verbose: bool = False, ptxas_info: bool = False) -> str:
+    """Compile every .cu under csrc/ (in parallel) and link the shared library; then the binding of the token calls, without which the
+    rest of the package works.  Returns the library's path."""
+    _build_library(verbose, ptxas_info)
+    try:
+        _build_binding(verbose)
+    except Exception as e:
+        raise RuntimeError(f"{LIB} is built, the binding of the token calls is not: {e}") from e
     return LIB
 
 
