@@ -63,8 +63,11 @@ int az_quantise_blocks(const void *x_dev, int x_type, int rows, int cols, int64_
  * codes with a scale for 128 x 128 (block_rows 128), i.e. a linear layer's weight as [out][in].  bias_dev: [n] float32
  * or NULL.  out_dev: [m][n] of out_type.  Sums are held in float32 and rounded once, when they are stored.  The order of
  * a sum depends on m, n and k only: equal calls give equal bits.
+ * A block's two scales are multiplied with each other first, in float32.  Where that product overflows (the largest values of the two
+ * blocks have a product above 448^2 x 2^128), the outputs of that row and those 128 columns are infinite or NaN, even where the
+ * block's sum is 0; a product below 2^-126 is rounded as a subnormal number, which moves the block's term by up to 2^-125.
  * k need not be a multiple of 128 (the last block is short); rows of a and b start on 16-byte boundaries, i.e. both
- * base addresses and both strides are multiples of 16.  a code of NaN (0x7f, 0xff) makes its outputs NaN.
+ * base addresses and both strides are multiples of 16.  A code of NaN (0x7f, 0xff) makes its outputs NaN.
  * A wait inside the kernel that runs out (none does, short of a fault) is reported by az_tokens_status.
  * Errors: BAD_ARG (null pointer, negative size, k == 0, unknown type, a stride smaller than a row, misaligned operand), UNSUPPORTED (a
  * size above 2^31 - 256), CUDA.  m == 0 or n == 0 is a no-op.

@@ -8,7 +8,7 @@ import time
 import pytest
 import torch
 
-from test_gpu_tokens import BF16, F32, TYPES, U, az, clean_status, gen, half_step, smallest  # noqa: F401
+from test_gpu_tokens import BF16, F32, TYPES, U, az, clean_status, dequantised, gen, half_step, smallest, up  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -175,3 +175,27 @@ def test_no_report_is_lost_between_streams(az, part):
     assert az.az_tokens_status() == 0
     with pytest.raises(az.AzError):
         az.az_selftest_tokens_timeout(2)
+
+
+# ---- products of scales beyond float32's range -----------------------------------------------------------------
+
+@pytest.mark.parametrize("m,n,k", [(1, 130, 512), (20, 20001, 300), (40, 300, 3000), (100, 300, 512), (100, 20001, 300), (400, 14100, 400)])
+def test_products_of_scales_beyond_float32(az, m, n, k):
+    """A pair whose product overflows reaches its row and its 128 columns, no others; products below 2^-126 keep fewer bits."""
+    g = gen(m + n + k)
+    codes = [torch.randint(0, 0x7f, (rows, up(k, 16)), generator=g, device="cuda", dtype=torch.uint8)[:, :k] for rows in (m, n)]
+    kb, nb = -(-k // 128), -(-n // 128)
+    sa = 2.0 ** -80 * (1 + torch.rand(m, kb, generator=g, device="cuda"))
+    sb = 2.0 ** -60 * (1 + torch.rand(nb, kb, generator=g, device="cuda"))
+    out = torch.empty(m, n, device="cuda")
+    az.az_block_matmul(codes[0], sa, codes[1], sb, out)
+    x, w = dequantised(codes[0], sa, 1), dequantised(codes[1], sb, 128)
+    want = x @ w.t()                                          # (all terms are positive: also the sum of magnitudes)
+    # a block's factor is off by up to 2^-150 there, its sum is at most 128 x 448 x 448 < 2^25
+    assert ((out.double() - want).abs() <= (256 + k / 128 + 12) * U * want + kb * 2.0 ** -125 + smallest(F32)).all()
+    row, block = m // 2, nb - 1
+    sa[row, 0], sb[block, 0] = 2.0 ** 66, 2.0 ** 66
+    az.az_block_matmul(codes[0], sa, codes[1], sb, out)
+    assert not out[row, block * 128:].isfinite().any()
+    out[row, block * 128:] = 0
+    assert out.isfinite().all()
