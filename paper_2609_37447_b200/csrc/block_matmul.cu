@@ -730,7 +730,13 @@ int launch(const void *a, int64_t a_stride, const void *b, int64_t b_stride, int
     //   2048 x 2048 x 2048 12.8 / 14.7, 1024 x 8192 x 2048 22.1 / 26.4, 8192^3 485 / 1445 (its first form);
     //   512 x 4096 x 4096 (32 tiles of pairs) 17.7 / 13.9, 1024 x 1858 x 2048 (32) 13.8 / 10.2;
     //   256 x 20000 x 4096 34.2 / 33.7, 300 x 40000 x 400 24.3 / 21.4, 129 x 20000 x 2048 21.7 / 20.3
-    const bool pair = args.m > 3 * kTileM && pairs * 8 >= sms * 3;
+    // 16-bit rows of an even length that is no multiple of eight are written two elements at a time by pairs and one by one by single:
+    // pairs for them from more than one tile of rows on.  us, pairs / single: 369 x 130374 x 577 80.0 / 98.4, 300 x 40002 x 400
+    // 27.7 / 34.4, 129 x 20002 x 2048 22.7 / 25.5, 380 x 50258 x 4096 105.5 / 105.9.  (Two at a time in single as well: 300 x 40002 x 400
+    // 23.4, but registers become tight and rows of an odd length, written one by one, go from 34.4 to 41 for 300 x 40001 x 400.)
+    const uintptr_t spread = reinterpret_cast<uintptr_t>(args.out) | (uintptr_t)(args.out_stride * 2);
+    const bool by_words = args.out_type != AZ_TYPE_F32 && (spread & 15) != 0 && (spread & 3) == 0;
+    const bool pair = args.m > (by_words ? 1 : 3) * kTileM && pairs * 8 >= sms * 3;
     // turned up to 64 rows, us for n x k, turned / single (131072 x 4096: held for half a second, the power limit reached):
     //   131072 x 4096   1 row 81.2 / 105.6, 32 rows 87.9 / 109.9, 64 rows 99.9 / 112.6, 77 rows (three pieces a part) 119.0 / 114.9
     //   20001 x 1000    5 rows 6.8 / 10.9, 33 rows 7.9 / 12.4, 64 rows 8.6 / 12.9;   4096 x 4096   1 row 6.7 / 7.4, 64 rows 9.1 / 10.2

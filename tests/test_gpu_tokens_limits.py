@@ -8,7 +8,8 @@ import time
 import pytest
 import torch
 
-from test_gpu_tokens import BF16, F32, TYPES, U, az, clean_status, dequantised, gen, half_step, smallest, up  # noqa: F401
+from test_gpu_tokens import (BF16, F32, TYPES, U, az, check_product, clean_status, dequantised, gen, half_step,  # noqa: F401
+                             operand, padded, smallest, up)
 
 pytestmark = pytest.mark.gpu
 
@@ -199,3 +200,23 @@ def test_products_of_scales_beyond_float32(az, m, n, k):
     assert not out[row, block * 128:].isfinite().any()
     out[row, block * 128:] = 0
     assert out.isfinite().all()
+
+
+# ---- rows of the product that are written two elements at a time -------------------------------------------------
+
+@pytest.mark.parametrize("m,n,k", [(129, 14402, 300), (300, 15002, 400), (369, 20006, 577), (384, 14340, 136), (128, 15002, 300)])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_rows_of_every_alignment_hold_the_same_bits(az, m, n, k, dtype):
+    """The form of the kernel goes by the rows' alignment too, the order of a sum does not."""
+    a, sa = operand(m, k, 1, 1)
+    b, sb = operand(n, k, 128, 2)
+    v = torch.randn(n, generator=gen(3), device="cuda")
+    outs = []
+    for stride, offset in ((up(n, 8), 0), (n, 0), (n + 2, 2), (n + 1, 1)):
+        flat, out = padded(m, n, stride, dtype, -7.0, offset)
+        az.az_block_matmul(a, sa, b, sb, out, bias=v)
+        rest = flat[offset:offset + m * stride].view(m, stride)[:, n:]
+        assert (rest == -7.0).all() and (flat[:offset] == -7.0).all() and (flat[offset + m * stride:] == -7.0).all()
+        outs.append(out)
+    assert all(torch.equal(outs[0], out) for out in outs)
+    check_product(az, m, n, k, dtype, True, 5)
