@@ -51,7 +51,7 @@ enum { AZ_TYPE_F32 = 0, AZ_TYPE_BF16 = 1, AZ_TYPE_F16 = 2 };
  * float32, row stride scales_stride.
  * No alignment is asked for beyond the element's own; 16-byte aligned rows are read and written fastest.
  * Errors: BAD_ARG (null pointer, negative size, unknown type, block_rows, a stride smaller than a row, misaligned
- * element), CUDA.  rows == 0 or cols == 0 is a no-op.
+ * element), UNSUPPORTED (more than about 2^44 elements), CUDA.  rows == 0 or cols == 0 is a no-op.
  */
 int az_quantise_blocks(const void *x_dev, int x_type, int rows, int cols, int64_t x_stride, int block_rows,
                        void *codes_dev, int64_t codes_stride, float *scales_dev, int64_t scales_stride, void *cuda_stream);
@@ -91,8 +91,8 @@ int az_block_matmul(const void *a_dev, int64_t a_stride, const float *a_scales_d
  * Bias lists are bias_tokens / bias_values[bias_offsets[r] .. bias_offsets[r + 1]), offsets clamped to [0, bias_count].
  * Allowed tokens: bit (t & 31) of word t >> 5 of the row's mask; bits beyond the vocabulary are ignored.  allowed_stride 0:
  * all rows share one mask.  The 64-bit masks of az_legal_masks are such masks with twice the words (a stride of 60 for the
- * flat head).  repetition and temperature are positive and finite; a row where they are not has unspecified values (what is not
- * allowed stays so).
+ * flat head).  repetition and temperature are positive, finite and no subnormal numbers (at least 2^-126: the reciprocal of a smaller
+ * temperature is infinite); a row where they are not has unspecified values (what is not allowed stays so).
  */
 typedef struct {
     const int32_t *tokens;           /* [rows][token_room], row stride token_stride */

@@ -8,10 +8,17 @@ import time
 import pytest
 import torch
 
-from test_gpu_tokens import (BF16, F32, TYPES, U, az, check_product, clean_status, dequantised, gen, half_step,  # noqa: F401
-                             operand, padded, smallest, up)
+from test_gpu_tokens import (BF16, F32, TYPES, U, az, check_logits, check_product, clean_status, dequantised, gen, half_step,  # noqa: F401
+                             operand, padded, reference, smallest, up)
 
 pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(autouse=True)
+def release_memory():
+    """Some tests hold tens of gigabytes; the next ones may run in other processes."""
+    yield
+    torch.cuda.empty_cache()
 
 
 # ---- logits: CTAs of a cluster whose share of the row holds nothing ------------------------------------------
@@ -220,3 +227,93 @@ def test_rows_of_every_alignment_hold_the_same_bits(az, m, n, k, dtype):
         outs.append(out)
     assert all(torch.equal(outs[0], out) for out in outs)
     check_product(az, m, n, k, dtype, True, 5)
+
+
+# ---- parameters at the ends of their types ---------------------------------------------------------------------
+
+@pytest.mark.parametrize("vocab", [1858, 9000, 131072])
+def test_the_lowest_and_highest_temperatures(az, vocab):
+    heat = torch.tensor([2.0 ** -126, 1e-37, 1e-30, 1.0, 1e30, torch.finfo(F32).max], device="cuda")
+    rows = len(heat)
+    logits = torch.randn(rows, vocab, generator=gen(vocab), device="cuda") * 3 - 20
+    probs, out = torch.empty_like(logits), torch.empty_like(logits)
+    best = torch.empty(rows, dtype=torch.int32, device="cuda")
+    logprob = torch.empty(rows, device="cuda")
+    az.az_token_probs(logits, probs, best, logprob, temperature=heat)
+    top = logits.argmax(1)
+    assert torch.equal(best.long(), top)
+    one = torch.nn.functional.one_hot(top[:3], vocab).to(F32)
+    assert torch.equal(probs[:3], one) and (logprob[:3] == 0).all()
+    # hot rows: every exponent is 0 up to 1e-29
+    assert ((probs[4:].double() * vocab - 1).abs() <= 120 * U).all()
+    assert ((logprob[4:].double() + math.log(vocab)).abs() <= 240 * U + 4 * U * math.log(vocab) + 1e-7).all()
+    az.az_adjust_logits(logits, out, temperature=heat)
+    want = logits.double() / heat.double()[:, None]
+    fine = want.abs() < 3e38
+    # (1 / T below the normal range: off by 2^-150, under 2^-20 of itself)
+    assert ((out.double() - want).abs()[fine] <= (2.0 ** -20 * want.abs() + smallest(F32))[fine]).all()
+    assert (out[~fine & (want < -3.5e38)] == -math.inf).all()
+
+
+@pytest.mark.parametrize("vocab", [1858, 9000, 131072])
+def test_tokens_lengths_and_offsets_at_the_ends_of_their_type(az, vocab):
+    """Ids outside the vocabulary are skipped and lengths and offsets clamped, be they the least or the greatest 32-bit numbers."""
+    low, high = -2 ** 31, 2 ** 31 - 1
+    rows, room = 6, 40
+    g = gen(vocab)
+    tokens = torch.randint(0, vocab, (rows, room), generator=g, device="cuda").int()
+    tokens[:, ::3] = torch.tensor([low, -1, vocab, vocab + 7, high - 7, high], device="cuda", dtype=torch.int32)[:, None]
+    lengths = torch.tensor([high, low, room, high, 17, room], device="cuda", dtype=torch.int32)
+    prompts = torch.tensor([low, high, 5, high, high, -1], device="cuda", dtype=torch.int32)
+    names = torch.tensor([low, 3, vocab - 1, vocab, high - 3, high, 8, 5, 9, 11], device="cuda", dtype=torch.int32)
+    values = torch.randn(len(names), generator=g, device="cuda")
+    rules = dict(tokens=tokens, lengths=lengths, prompt_lengths=prompts, repetition=torch.full((rows,), 1.3, device="cuda"),
+                 presence=torch.full((rows,), 0.5, device="cuda"), frequency=torch.full((rows,), 0.25, device="cuda"))
+    logits = torch.randn(rows, vocab, generator=g, device="cuda") * 4
+    plain = dict(rules, bias_offsets=torch.tensor([0, 8, 10, 10, 10, 10, 10], device="cuda", dtype=torch.int32), bias_tokens=names,
+                 bias_values=values)
+    want = reference(logits, plain)
+    check_logits(az, logits, plain, want=want)
+    wild = dict(plain, bias_offsets=torch.tensor([low, 8, high, high, low, low, high], device="cuda", dtype=torch.int32))
+    # rows 0, 1: as above; row 2: high .. high, 3: high .. low, 4: low .. low: nothing; row 5: all of the list
+    want = reference(logits, dict(rules, bias_offsets=torch.tensor([0, 8, 10, 10, 10, 10, 20], device="cuda", dtype=torch.int32),
+                                  bias_tokens=torch.cat([names, names]), bias_values=torch.cat([values, values])))
+    check_logits(az, logits, wild, want=want)
+
+
+@pytest.mark.parametrize("wide", [False, True])
+def test_the_largest_products(az, wide):
+    """2^31 - 256 rows, and as many columns: every output, at its place."""
+    most, k = 2 ** 31 - 256, 16
+    long, one = torch.full((most, k), 0x38, dtype=torch.uint8, device="cuda"), torch.full((1, k), 0x40, dtype=torch.uint8, device="cuda")     # 1.0 and 2.0
+    long[::1000003] = 0x30                                    # 0.5
+    step = 128 if wide else 1
+    scales = torch.ones((-(-most // step), 1), device="cuda")
+    scales[-1] = 4.0
+    unit = torch.ones((1, 1), device="cuda")
+    out = torch.full((1, most) if wide else (most, 1), -7.0, device="cuda", dtype=BF16)
+    if wide:
+        az.az_block_matmul(one, unit, long, scales, out)
+    else:
+        az.az_block_matmul(long, scales, one, unit, out)
+    flat = out.view(-1)
+    flat[most - step:] /= 4.0
+    assert (flat[::1000003] == 16.0).all()
+    flat[::1000003] = 32.0
+    assert (flat == 32.0).all()
+
+
+def test_the_largest_number_of_quantised_rows(az):
+    rows = 2 ** 31 - 1
+    x = torch.full((rows, 1), 2.0, device="cuda", dtype=BF16)
+    x[::1000003] = 0.0
+    codes = torch.full((rows, 1), 0x55, device="cuda", dtype=torch.uint8)
+    scales = torch.full((rows, 1), -7.0, device="cuda")
+    az.az_quantise_blocks(x, codes, scales, 1)
+    assert (scales[::1000003] == 2.0 ** -126).all() and ((codes[::1000003] & 0x7f) == 0).all()
+    scales[::1000003], codes[::1000003] = 2.0 / 448, 0x7e
+    assert (scales == 2.0 / 448).all() and (codes == 0x7e).all()
+    few = scales[: -(-rows // 128)]
+    few.fill_(-7.0)
+    az.az_quantise_blocks(x, codes, few, 128)
+    assert (few == 2.0 / 448).all() and (codes[1::1000003] == 0x7e).all() and ((codes[::1000003] & 0x7f) == 0).all()

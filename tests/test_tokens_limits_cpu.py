@@ -16,6 +16,13 @@ def test_the_status_self_test_knows_two_parts():
     assert az._lib.az_selftest_tokens_timeout(-1, None) == az.AZ_ERR_BAD_ARG
 
 
+@pytest.mark.parametrize("block_rows", [1, 128])
+def test_quantise_refuses_more_blocks_than_a_grid_holds(block_rows):
+    most, address = 2 ** 31 - 1, 1 << 20
+    assert az._lib.az_quantise_blocks(address, az.AZ_TYPE_BF16, most, most, most, block_rows, address, most, address, 1 << 24,
+                                      None) == az.AZ_ERR_UNSUPPORTED
+
+
 def test_the_package_without_the_binding_of_the_token_calls():
     """The engine's calls work; the token calls say what is missing, each time."""
     code = """
