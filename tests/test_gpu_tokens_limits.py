@@ -8,7 +8,7 @@ import time
 import pytest
 import torch
 
-from test_gpu_tokens import (BF16, F32, TYPES, U, az, check_logits, check_product, clean_status, dequantised, gen, half_step,  # noqa: F401
+from test_gpu_tokens import (BF16, F16, F32, TYPES, U, az, check_logits, check_product, clean_status, dequantised, gen, half_step,  # noqa: F401
                              operand, padded, reference, smallest, up)
 
 pytestmark = pytest.mark.gpu
@@ -317,3 +317,41 @@ def test_the_largest_number_of_quantised_rows(az):
     few.fill_(-7.0)
     az.az_quantise_blocks(x, codes, few, 128)
     assert (few == 2.0 / 448).all() and (codes[1::1000003] == 0x7e).all() and ((codes[::1000003] & 0x7f) == 0).all()
+
+
+# ---- the quantiser's quotients -----------------------------------------------------------------------------------
+
+def codes_by_definition(x, scale):
+    """|x| / scale rounded once to e4m3, as code magnitudes, by comparison with the middles between codes (float64, on the GPU)."""
+    grid = torch.arange(127, dtype=torch.uint8, device="cuda").view(torch.float8_e4m3fn).double()
+    middle = (grid[1:] + grid[:-1]) / 2
+    ratio = x.double().abs() / scale.double()
+    low, high = torch.bucketize(ratio, middle), torch.bucketize(ratio, middle, right=True)
+    return torch.where(low % 2 == 0, low, high)
+
+
+@pytest.mark.parametrize("dtype,mantissa", [(F16, 10), (BF16, 7)])
+@pytest.mark.parametrize("exponent", ["lowest", "low", "one", "highest"])
+def test_every_16_bit_number_under_every_maximum(az, dtype, mantissa, exponent):
+    """Each 16-bit magnitude in a block with each mantissa of a maximum: the codes are those of the real quotients."""
+    info = torch.finfo(dtype)
+    first = {"lowest": 1, "low": (torch.tensor(info.smallest_normal, dtype=dtype).view(torch.int16).item()),
+             "one": torch.tensor(1.0, dtype=dtype).view(torch.int16).item(),
+             "highest": torch.tensor(info.max, dtype=dtype).view(torch.int16).item() - (1 << mantissa) + 1}[exponent]
+    tops = torch.arange(first, first + (1 << mantissa), device="cuda")
+    # magnitudes within 2^16 of the maximum: smaller ones have the code 0
+    reach = 16 << mantissa
+    offsets = torch.arange(-reach, 1 << mantissa, device="cuda")
+    per_row = -(-len(offsets) // 127)
+    offsets = torch.nn.functional.pad(offsets, (0, per_row * 127 - len(offsets)))
+    for some in tops.split(max(1, (1 << 25) // len(offsets))):
+        bits = (some[:, None] + offsets).clamp_min(0)
+        bits = torch.where(bits > some[:, None], 0, bits).view(len(some), per_row, 127)
+        bits = torch.cat([bits, some[:, None, None].expand(-1, per_row, 1)], 2).view(len(some), per_row * 128)
+        x = bits.to(torch.int16).view(dtype)
+        codes, scales = torch.empty(x.shape, dtype=torch.uint8, device="cuda"), torch.empty(len(some), per_row, device="cuda")
+        az.az_quantise_blocks(x, codes, scales, 1)
+        top = some.to(torch.int16).view(dtype).double()
+        want = torch.maximum((top / 448).float(), torch.tensor(2.0 ** -126, device="cuda"))
+        assert (scales == want[:, None]).all()
+        assert torch.equal((codes & 0x7f).long(), codes_by_definition(x, want[:, None]))
