@@ -573,7 +573,17 @@ __global__ void __launch_bounds__(kThreads, kItems > 4 ? 1 : 1024 / kThreads) lo
             __syncthreads();
             whole = row_part;
             // (a slice with nothing above -infinity has exponentials of 0 and no max to compare: base is 0 there, far above a low row max)
-            factor = mine.top == -INFINITY ? 0.0f : exp2_approx((base - whole.top) * scale);
+            const float below = (mine.top == -INFINITY ? -INFINITY : base - whole.top) * scale;
+            factor = exp2_approx(below);
+            // a slice far below the row's max: its factor over the sum would be a subnormal number, so the exponentials hand their 2^24
+            // to the factor (they lose bits below 2^-126 then, where the probability is below 2^-190)
+            if (factor < 0x1p-64f) {
+                factor = exp2_approx(below + 24.0f);
+#pragma unroll
+                for (int i = 0; i < kItems; ++i)
+#pragma unroll
+                    for (int j = 0; j < kPer; ++j) x[i][j] *= 0x1p-24f;
+            }
         }
         const bool empty = whole.top == -INFINITY;
         if (rank == 0 && tid == 0) {

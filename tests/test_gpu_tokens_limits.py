@@ -355,3 +355,21 @@ def test_every_16_bit_number_under_every_maximum(az, dtype, mantissa, exponent):
         want = torch.maximum((top / 448).float(), torch.tensor(2.0 ** -126, device="cuda"))
         assert (scales == want[:, None]).all()
         assert torch.equal((codes & 0x7f).long(), codes_by_definition(x, want[:, None]))
+
+
+# ---- probabilities near the end of float32 ---------------------------------------------------------------------
+
+@pytest.mark.parametrize("kind", [F32, BF16])
+@pytest.mark.parametrize("rows,vocab", [(4, 1858), (4, 9000), (4, 40000), (3, 131072), (200, 20000)])
+def test_small_probabilities_of_slices_far_below_the_best(az, kind, rows, vocab):
+    """Chunks of the row whose best tokens have probabilities from 1 down to nothing: each right to the last number of its type."""
+    g = gen(vocab)
+    chunk = torch.arange(vocab, device="cuda") // 256
+    level = -106 * torch.rand((rows, int(chunk[-1]) + 1), generator=g, device="cuda")
+    level[:, 0] = 0.0
+    heat = torch.tensor([1.0, 0.05, 0.7, 0.01], device="cuda")[torch.arange(rows, device="cuda") % 4]
+    logits = level[:, chunk] - torch.rand((rows, vocab), generator=g, device="cuda")
+    for slices in (1, 8):                                     # neighbouring chunks alike: whole slices far below
+        some = level[:, (chunk % slices)] - torch.rand((rows, vocab), generator=g, device="cuda") if slices > 1 else logits
+        check_logits(az, ((some - 3.0) * heat[:, None]).to(kind), {"temperature": heat}, F32)
+        check_logits(az, ((some - 3.0) * heat[:, None]).to(kind), {"temperature": heat}, kind)
