@@ -373,3 +373,51 @@ def test_small_probabilities_of_slices_far_below_the_best(az, kind, rows, vocab)
         some = level[:, (chunk % slices)] - torch.rand((rows, vocab), generator=g, device="cuda") if slices > 1 else logits
         check_logits(az, ((some - 3.0) * heat[:, None]).to(kind), {"temperature": heat}, F32)
         check_logits(az, ((some - 3.0) * heat[:, None]).to(kind), {"temperature": heat}, kind)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("vocab", [300, 1858, 9001, 40000, 131072])
+@pytest.mark.parametrize("rows", [12, 300])
+def test_infinities_and_nan_anywhere_in_a_row(az, dtype, vocab, rows):
+    """One to three odd values in each row, allowed or not, wherever the row is cut."""
+    if rows * vocab > 1 << 24:
+        rows = 60
+    g = gen(vocab + rows)
+    logits = (torch.randn(rows, vocab, generator=g, device="cuda") * 3 - 50).to(dtype)
+    at = torch.randint(0, vocab, (rows, 3), generator=g, device="cuda")
+    kinds = torch.tensor([math.nan, math.inf, -math.inf, -1000.0], device="cuda", dtype=dtype)
+    logits.scatter_(1, at, kinds[torch.randint(0, 4, (rows, 3), generator=g, device="cuda")])
+    open_ = torch.rand(rows, vocab, generator=g, device="cuda") < torch.tensor([0.5, 0.003, 1.0], device="cuda")[torch.arange(rows, device="cuda") % 3][:, None]
+    open_[::4, at[0]] = True
+    open_[1::7] = False
+    words = -(-vocab // 32)
+    bits = torch.nn.functional.pad(open_, (0, words * 32 - vocab)).view(rows, words, 32).long() << torch.arange(32, device="cuda")
+    packed = bits.sum(-1)
+    allowed = torch.where(packed >= 2 ** 31, packed - 2 ** 32, packed).int()
+    heat = 0.02 + torch.rand(rows, generator=g, device="cuda")
+    probs = torch.full((rows, vocab), -1.0, device="cuda")
+    best = torch.empty(rows, dtype=torch.int32, device="cuda")
+    logprob = torch.empty(rows, device="cuda")
+    az.az_token_probs(logits, probs, best, logprob, allowed=allowed, temperature=heat)
+    out = torch.empty_like(logits)
+    az.az_adjust_logits(logits, out, allowed=allowed)
+    assert torch.equal(out.nan_to_num(nan=7.0, posinf=8.0, neginf=9.0),
+                       torch.where(open_, logits, -math.inf).nan_to_num(nan=7.0, posinf=8.0, neginf=9.0))
+    line = torch.where(open_, logits.double(), -math.inf)
+    nan = line.isnan().any(1)
+    odd = nan | (line == math.inf).any(1)
+    empty = ~odd & (line == -math.inf).all(1)
+    assert odd.any() and empty.any() and (~odd & ~empty).any()
+    assert (probs[~open_] == 0).all() and (probs[empty] == 0).all()
+    assert probs[odd][open_[odd]].isnan().all() and logprob[odd].isnan().all()
+    assert (best[empty] == -1).all() and (logprob[empty] == -math.inf).all()
+    place = torch.arange(vocab, device="cuda")
+    top = line.nan_to_num(nan=-math.inf, posinf=math.inf, neginf=-math.inf).amax(1, keepdim=True)
+    is_top = torch.where(nan[:, None], line.isnan(), line == top)
+    lowest = torch.where(is_top & open_, place, vocab).amin(1)
+    assert torch.equal(best.long()[~empty], lowest[~empty])
+    fine = ~odd & ~empty
+    x = (line - top) / heat.double()[:, None]
+    want = x.exp() / x.exp().sum(1, keepdim=True)
+    rel = (12 * 100 / heat.double()[:, None] + 5 * x.abs().clamp_max(1e4) + 120) * U
+    assert ((probs.double() - want).abs() <= (rel + U) * want + smallest(F32))[fine].all()
