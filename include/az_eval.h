@@ -379,8 +379,8 @@ int az_tower_time(az_net *net, float *total_ms_out, int *passes_out);
 
 /*
  * Self-test of the failure path: launches a one-CTA kernel whose warps wait, through the same
- * bounded wait as the tensor-core kernels, on a barrier nothing ever arrives on (poll limit a few
- * tens of microseconds).  Returns AZ_ERR_DEVICE_TIMEOUT when the wait ran out, the kernel raised its
+ * bounded wait as the tensor-core kernels, on a barrier nothing ever arrives on (the polls run out
+ * after about 70 ms).  Returns AZ_ERR_DEVICE_TIMEOUT when the wait ran out, the kernel raised its
  * status bit and still left through its normal teardown -- i.e. when failure detection works --
  * and AZ_OK / another error otherwise.  Nothing hangs or traps; the context stays usable.
  */

@@ -1,8 +1,8 @@
 /*
  * az_tokens -- the output end of a language model on one NVIDIA B200 (sm_100a), from hidden states to the
- * probabilities of the next token.  It is the path that az_evaluate's policy head takes for the moves of a
- * position (features -> matrix product -> logits -> softmax over the entries a bit mask allows), for
- * vocabularies of 10^5 entries and operands of 8 bits:
+ * probabilities of the next token.  It takes the steps that az_evaluate's policy head takes for the moves of a
+ * position (features -> matrix product -> logits -> softmax over the entries a bit mask allows) with kernels of
+ * its own, for vocabularies of 10^5 entries and operands of 8 bits; az_evaluate does not call it:
  *
  *   hidden states   --az_quantise_blocks-->  e4m3 codes with one scale for each block of 128
  *   codes, weights  --az_block_matmul----->  logits

@@ -11,10 +11,11 @@
 // TMEM holds two blocks of 256 columns; so that the tensor cores wait little, a block is two products of 128 columns, each with its
 // own "done" and "free" (a slot), the slot is free as soon as its last columns are in registers, scales are in registers
 // before the block is done, and signals are single predicated instructions.
-// Measured: 8192^3 460 to 545 us (2.0 to 2.4 PFLOP/s, as far as the SM clock falls under power: 1.4 to 1.6 GHz; a library product
-// with ONE scale for each operand, which has nothing to add up, takes 362), 77 x 131072 x 4096 96 us (5.8 TB/s, 88 % of
-// the measured copy bandwidth), 1024 x 1858 x 2048 with float32 results 10.4 us (operands from L2: 63 bytes a cycle and SM),
-// 1 x 131072 x 4096 81 us (6.6 TB/s), 1 x 4096 x 4096 6.3 us (launch, first copies and the exchange).
+// Measured on the device, a dozen calls in a graph: 8192^3 470 to 550 us (2.0 to 2.3 PFLOP/s, as far as the SM clock falls under
+// power: 1.4 to 1.6 GHz; a library product with ONE scale for each operand, which has nothing to add up, takes 362), 77 x 131072 x
+// 4096 94 to 98 us (5.7 to 5.9 TB/s, 87 to 90 % of the measured copy bandwidth), 1024 x 1858 x 2048 with float32 results 10.3 us
+// (operands from L2: 63 bytes a cycle and SM), 1 x 131072 x 4096 81 us (6.6 TB/s), 1 x 4096 x 4096 6.3 us (launch, first copies and
+// the exchange).  Call after call for seconds, at the power limit: 8192^3 546 us, 77 x 131072 x 4096 114 us (4.9 TB/s).
 //
 // Operands come by TMA (128-byte swizzle: a tile row is exactly one block of k).  Rows and columns beyond the matrices are
 // filled with zeros by the copy.  A tile of a is as many rows as there are (rounded up to sixteen, at most 128): rows of the
@@ -315,8 +316,8 @@ block_matmul_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
                 int row_a, row_b;
                 place<kRows, kCols>(args, tile, row_a, row_b);
                 if (kPair) { row_a += rank * kTileM; row_b += rank * (kTileM / kSlotsPerBlock); }
-    #pragma unroll 1
-            for (int c = c_begin; c < c_end; ++c) {
+#pragma unroll 1
+                for (int c = c_begin; c < c_end; ++c) {
                     ok = bounded_wait(bar_empty(s), phase ^ 1u, abort_flag, &g_status, kStatusWaitTimeout, kSpinLimit);
                     if (!ok) break;
                     if (lane == 0) {
@@ -324,8 +325,8 @@ block_matmul_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
                         ptx::mbar_arrive_expect_tx(bar_full(s), stage_bytes);
                         tma_load(at, &map_a, c * kBlockK, row_a, bar_full(s));
                         // (pair: this CTA's rows of b are half of each slot's columns, so that a slot is 128 neighbouring columns)
-                    for (int h = 0; h < kSlotsPerBlock; ++h)
-                        tma_load(at + a_bytes + (uint32_t)(h * (kTileM / kSlotsPerBlock) * kBlockK), &map_b, c * kBlockK, row_b + h * kSlotCols, bar_full(s));
+                        for (int h = 0; h < kSlotsPerBlock; ++h)
+                            tma_load(at + a_bytes + (uint32_t)(h * (kTileM / kSlotsPerBlock) * kBlockK), &map_b, c * kBlockK, row_b + h * kSlotCols, bar_full(s));
                     }
                     if (++s == args.stages) { s = 0; phase ^= 1u; }
                     __syncwarp();
@@ -342,8 +343,8 @@ block_matmul_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
             int s = 0;
             uint32_t phase = 0;
             for (int tile = first_tile; tile < args.tiles && ok; tile += tile_step)
-    #pragma unroll 1
-            for (int c = c_begin; c < c_end; ++c) {
+#pragma unroll 1
+                for (int c = c_begin; c < c_end; ++c) {
                     ok = bounded_wait(bar_full(s), phase, abort_flag, &g_status, kStatusWaitTimeout, kSpinLimit);
                     if (!ok) break;
                     if (lane == 0) ptx::mbar_arrive_cluster_relaxed(ptx::map_to_cta(bar_peer(s), 0));
@@ -360,8 +361,8 @@ block_matmul_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
             int s = 0, t = 0;
             uint32_t phase = 0, t_phase = 0;
             for (int tile = first_tile; tile < args.tiles && ok; tile += tile_step)
-    #pragma unroll 1
-            for (int c = c_begin; c < c_end; ++c) {
+#pragma unroll 1
+                for (int c = c_begin; c < c_end; ++c) {
                     ok = bounded_wait(bar_full(s), phase, abort_flag, &g_status, kStatusWaitTimeout, kSpinLimit);
                     if (kPair) ok = ok && bounded_wait<true>(bar_peer(s), phase, abort_flag, &g_status, kStatusWaitTimeout, kSpinLimit);
                     const uint32_t at = tiles_at + (uint32_t)s * stage_bytes;
@@ -477,11 +478,11 @@ block_matmul_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
                 const bool live = m0 < args.m;                         // of the whole warp
                 const int col0 = n0 + part_n * kSumCols;
                 if (args.bias && part == 0 && live) {
-    #pragma unroll
+#pragma unroll
                     for (int j = 0; j < kSumCols / 2; ++j)
                         acc[j] = make_float2(args.bias[min(col0 + 2 * j, args.n - 1)], args.bias[min(col0 + 2 * j + 1, args.n - 1)]);
                 } else {
-    #pragma unroll
+#pragma unroll
                     for (int j = 0; j < kSumCols / 2; ++j) acc[j] = make_float2(0.0f, 0.0f);
                 }
                 for (int c0 = c_begin; c0 < c_end && ok; c0 += kScaleBlocks) {
@@ -491,13 +492,13 @@ block_matmul_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
                     {
                         const float *sa = scales + u * kScaleFloats + quarter * 32 + lane;
                         const float *sb = scales + u * kScaleFloats + kScaleBlocks * kScalePitch + (part_n * kSumCols / kBlockK) * kScaleBlocks;
-    #pragma unroll
+#pragma unroll
                         for (int i = 0; i < kScaleBlocks; ++i) factor[i] = sa[i * kScalePitch] * sb[i];
                     }
                     __syncwarp();
                     arrive_if(first_lane, bar_scales_free(u));
                     if (++u == kBuffers) { u = 0; u_phase ^= 1u; }
-    #pragma unroll
+#pragma unroll
                     for (int i = 0; i < kScaleBlocks; ++i) {
                         if (c0 + i >= c_end) break;
                         ok = __all_sync(0xffffffffu, ptx::mbar_try_wait(bar_done(t), t_phase)) ||
@@ -510,7 +511,7 @@ block_matmul_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
                         if (live) {
                             ptx::tmem_ld16(at, d[0]);
                             ptx::tmem_ld_wait();
-    #pragma unroll
+#pragma unroll
                             for (int j = 0; j + 16 < kSumCols; j += 16) {
                                 ptx::tmem_ld16(at + (uint32_t)(j + 16), d[(j / 16 + 1) & 1]);
                                 add_columns<16>(d[(j / 16) & 1], scale, acc + j / 2);
@@ -540,7 +541,7 @@ block_matmul_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
                 ptx::cluster_wait();                        // every CTA of the cluster runs
                 if (quarter * 32 + lane < rows) {
                     const uint32_t here = ptx::smem_addr(exchange) + (uint32_t)((rank * args.a_rows + quarter * 32 + lane) * pitch) * 4u;
-    #pragma unroll
+#pragma unroll
                     for (int j = 0; j < kSumCols; j += 4) {
                         const int col = part_n * kSumCols + j;
                         ptx::st_cluster_v4(ptx::map_to_cta(here + (uint32_t)(col & (width - 1)) * 4u, (uint32_t)(col >> args.width_log2)),

@@ -19,7 +19,8 @@
 // 8192 x 8192 instead of 39.4).
 //
 // Bound by instruction issue and HBM about alike: a block is read once, held in registers and written once.  8192 x 8192 bf16:
-// 39.4 us, 5.2 TB/s (79 % of the measured copy bandwidth); 128 x 128 blocks of 11003 x 4100 float32: 41.2 us, 5.5 TB/s (84 %).
+// 39.3 us, 5.2 TB/s (79 % of the measured copy bandwidth); 128 x 128 blocks of 11003 x 4100 float32: 40.7 us, 5.5 TB/s (84 %); on the
+// device, in a graph of calls.  Call by call, into outputs allocated each time: 41.7 and 44.9 us.
 #include "common.cuh"
 #include "ptx.cuh"
 
@@ -40,7 +41,7 @@ __device__ __forceinline__ float to_f32(float v) { return v; }
 __device__ __forceinline__ float to_f32(__nv_bfloat16 v) { return __bfloat162float(v); }
 __device__ __forceinline__ float to_f32(__half v) { return __half2float(v); }
 
-// Eight elements of a row's block, as they are stored.  kVec: consecutive ones from 16-byte loads; else every eighth,
+// Sixteen elements of a row's block, as they are stored.  kVec: consecutive ones from 16- or 32-byte loads; else every eighth,
 // one by one.
 template <typename T, bool kVec>
 struct Slice {
