@@ -7,15 +7,16 @@
 // own read it back, multiply it by the block's scales and add it up in registers while the tensor cores are at the next block.
 // A thread holds one row of the tile, so a block costs it one scale and one fused multiply-add per column (turned: below).
 //
-// What bounds the large form is the way of a block's columns around: product, "done", read and add up, "free", next product.
+// What the large form waits for is the way of a block's columns around (product, "done", read and add up, "free", next product) and
+// the clock under the power limit; how much for each has not been measured apart (the tensor pipe is 50 % active without the limit).
 // TMEM holds two blocks of 256 columns; so that the tensor cores wait little, a block is two products of 128 columns, each with its
 // own "done" and "free" (a slot), the slot is free as soon as its last columns are in registers, scales are in registers
 // before the block is done, and signals are single predicated instructions.
 // Measured on the device, a dozen calls in a graph: 8192^3 470 to 550 us (2.0 to 2.3 PFLOP/s, as far as the SM clock falls under
 // power: 1.4 to 1.6 GHz; a library product with ONE scale for each operand, which has nothing to add up, takes 362), 77 x 131072 x
 // 4096 94 to 98 us (5.7 to 5.9 TB/s, 87 to 90 % of the measured copy bandwidth), 1024 x 1858 x 2048 with float32 results 10.3 us
-// (operands from L2: 63 bytes a cycle and SM), 1 x 131072 x 4096 81 us (6.6 TB/s), 1 x 4096 x 4096 6.3 us (launch, first copies and
-// the exchange).  Call after call for seconds, at the power limit: 8192^3 546 us, 77 x 131072 x 4096 114 us (4.9 TB/s).
+// (operands from L2: 63 bytes a cycle and SM), 1 x 131072 x 4096 81 to 85 us (6.3 to 6.6 TB/s), 1 x 4096 x 4096 6.3 us (launch, first
+// copies and the exchange).  Call after call for seconds, at the power limit: 8192^3 546 us, 77 x 131072 x 4096 114 us (4.9 TB/s).
 //
 // Operands come by TMA (128-byte swizzle: a tile row is exactly one block of k).  Rows and columns beyond the matrices are
 // filled with zeros by the copy.  A tile of a is as many rows as there are (rounded up to sixteen, at most 128): rows of the

@@ -24,8 +24,8 @@
 // What bounds it: a row is a chain of latencies (parameters, history, biases, two barriers, the exchange), and two CTAs of an SM are all
 // that there is to fill them.  Clusters stay for several rows: a row's logits, its parameters, mask, the first of its history
 // and of its biases are copied into shared memory while the one before is worked on, and words and bits are cleared by those who take
-// them over.  us on the device, in a graph of calls: 512 x 131072 bf16 162 to 177 with everything on (1.6 TB/s), 77 without rules
-// (3.5 TB/s); 256 x 100277 bf16 adjusted 90 (30 without rules); 1 x 131072 with 30,000 tokens of history 16; 1024 x 1858 float32 with
+// them over.  us on the device, in a graph of calls: 512 x 131072 bf16 162 to 177 with everything on (1.6 TB/s), 83 without rules
+// (3.2 TB/s); 256 x 100277 bf16 adjusted 90 (32 without rules); 1 x 131072 with 30,000 tokens of history 16; 1024 x 1858 float32 with
 // masks 7.2 (call by call, with three outputs to allocate, 9.0).
 #include "common.cuh"
 #include "ptx.cuh"
