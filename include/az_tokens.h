@@ -70,7 +70,7 @@ int az_quantise_blocks(const void *x_dev, int x_type, int rows, int cols, int64_
  * base addresses and both strides are multiples of 16.  A code of NaN (0x7f, 0xff) makes its outputs NaN.
  * A wait inside the kernel that runs out (none does, short of a fault) is reported by az_tokens_status.
  * Errors: BAD_ARG (null pointer, negative size, k == 0, unknown type, a stride smaller than a row, misaligned operand), UNSUPPORTED (a
- * size above 2^31 - 256), CUDA.  m == 0 or n == 0 is a no-op.
+ * size above 2^31 - 256, 2^46 outputs or more), CUDA.  m == 0 or n == 0 is a no-op.
  */
 int az_block_matmul(const void *a_dev, int64_t a_stride, const float *a_scales_dev, int64_t a_scales_stride,
                     const void *b_dev, int64_t b_stride, const float *b_scales_dev, int64_t b_scales_stride,

@@ -746,7 +746,6 @@ int launch(const void *a, int64_t a_stride, const void *b, int64_t b_stride, int
     const int tile = pair ? 256 : 128;
     args.tiles_m = (int)(((int64_t)args.m + tile - 1) / tile);
     args.tiles_n = (int)(((int64_t)args.n + tile - 1) / tile);
-    if ((pair ? pairs : singles) > 0x3fffffff) return AZ_ERR_UNSUPPORTED;
     args.tiles = (int)(pair ? pairs : singles);
     args.a_rows = args.m >= kTileM ? kTileM : (args.m + kPiece - 1) / kPiece * kPiece;
     // a cluster per tile, up to eight CTAs, as long as all clusters run at once (of eight CTAs 15 do, not 148 / 8; with
@@ -802,6 +801,8 @@ extern "C" int az_block_matmul(const void *a_dev, int64_t a_stride, const float 
     if (m < 0 || n < 0 || k <= 0 || out_type < AZ_TYPE_F32 || out_type > AZ_TYPE_F16) return AZ_ERR_BAD_ARG;
     if (m == 0 || n == 0) return AZ_OK;
     if (m > az::kMaxExtent || n > az::kMaxExtent || k > az::kMaxExtent) return AZ_ERR_UNSUPPORTED;
+    // (tiles are counted in 32 bits: of 256 x 256 where there are so many, at most 3 x 2^24 of 128 x 128 where there are 384 rows or fewer)
+    if ((((int64_t)m + 255) / 256) * (((int64_t)n + 255) / 256) > 0x3fffffff) return AZ_ERR_UNSUPPORTED;
     if (!a_dev || !a_scales_dev || !b_dev || !b_scales_dev || !out_dev) return AZ_ERR_BAD_ARG;
     const uintptr_t element = out_type == AZ_TYPE_F32 ? 4 : 2;
     if ((reinterpret_cast<uintptr_t>(a_dev) & 15) || (reinterpret_cast<uintptr_t>(b_dev) & 15) ||

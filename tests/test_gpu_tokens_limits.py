@@ -9,7 +9,7 @@ import pytest
 import torch
 
 from test_gpu_tokens import (BF16, F16, F32, TYPES, U, az, check_logits, check_product, clean_status, dequantised, gen, half_step,  # noqa: F401
-                             operand, padded, reference, smallest, up)
+                             make_rules, operand, padded, reference, smallest, up)
 
 pytestmark = pytest.mark.gpu
 
@@ -421,3 +421,15 @@ def test_infinities_and_nan_anywhere_in_a_row(az, dtype, vocab, rows):
     want = x.exp() / x.exp().sum(1, keepdim=True)
     rel = (12 * 100 / heat.double()[:, None] + 5 * x.abs().clamp_max(1e4) + 120) * U
     assert ((probs.double() - want).abs() <= (rel + U) * want + smallest(F32))[fine].all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("offset,more", [(1, 0), (0, 1), (3, 5)])
+def test_the_largest_vocabulary_at_any_alignment(az, dtype, offset, more):
+    """Rows that take one chunk more than 16 CTAs of the usual share hold."""
+    vocab, rows = 262144, 5
+    flat = (torch.randn(offset + rows * (vocab + more), generator=gen(more + 7), device="cuda") * 4).to(dtype)
+    logits = flat[offset:].view(rows, vocab + more)[:, :vocab]
+    rules = make_rules(rows, vocab, 3, history=900, biases=60)
+    check_logits(az, logits, rules, F32, vocab + more, offset)
+    check_logits(az, logits, {"allowed": rules["allowed"]}, None, vocab + 8, 0)

@@ -23,6 +23,13 @@ def test_quantise_refuses_more_blocks_than_a_grid_holds(block_rows):
                                       None) == az.AZ_ERR_UNSUPPORTED
 
 
+def test_product_refuses_more_tiles_than_it_counts():
+    """Before any CUDA call: here there is no device to ask."""
+    address, side, k = 1 << 20, 1 << 24, 16
+    assert az._lib.az_block_matmul(address, k, address, 1, address, k, address, 1, None, side, side, k, address, az.AZ_TYPE_F32, side,
+                                   None) == az.AZ_ERR_UNSUPPORTED
+
+
 def test_the_package_without_the_binding_of_the_token_calls():
     """The engine's calls work; the token calls say what is missing, each time."""
     code = """
