@@ -2,6 +2,9 @@
 the limits of their types.  Statements in 64 bits and tolerances as in test_gpu_tokens.py."""
 import ctypes
 import math
+import os
+import subprocess
+import sys
 import threading
 import time
 
@@ -433,3 +436,46 @@ def test_the_largest_vocabulary_at_any_alignment(az, dtype, offset, more):
     rules = make_rules(rows, vocab, 3, history=900, biases=60)
     check_logits(az, logits, rules, F32, vocab + more, offset)
     check_logits(az, logits, {"allowed": rules["allowed"]}, None, vocab + 8, 0)
+
+
+def test_first_calls_from_several_threads_at_once():
+    """The library's calls without the interpreter's lock, on a stream for each thread, from the process's first call on."""
+    code = """
+import ctypes, threading, torch
+import paper_2609_37447_b200 as az
+n, k, m, vocab = 9000, 512, 150, 9000
+torch.manual_seed(1)
+x, w = torch.randn(m, k, device="cuda"), torch.randn(n, k, device="cuda")
+p = lambda t: t.data_ptr()
+def chain(stream, out):
+    xq, xs, wq, ws, y, pr, best, lp = out
+    s = stream.cuda_stream
+    codes = [az._lib.az_quantise_blocks(p(w), 0, n, k, k, 128, p(wq), k, p(ws), 4, s), az._lib.az_quantise_blocks(p(x), 0, m, k, k, 1, p(xq), k, p(xs), 4, s),
+             az._lib.az_block_matmul(p(xq), k, p(xs), 4, p(wq), k, p(ws), 4, None, m, n, k, p(y), 0, n, s),
+             az._lib.az_token_probs(p(y), 0, m, vocab, n, None, p(pr), 0, n, p(best), p(lp), s)]
+    assert codes == [0, 0, 0, 0], codes
+def buffers():
+    u8 = dict(dtype=torch.uint8, device="cuda")
+    return [torch.empty(m, k, **u8), torch.empty(m, 4, device="cuda"), torch.empty(n, k, **u8), torch.empty(71, 4, device="cuda"),
+            torch.empty(m, n, device="cuda"), torch.empty(m, n, device="cuda"), torch.empty(m, dtype=torch.int32, device="cuda"), torch.empty(m, device="cuda")]
+streams = [torch.cuda.Stream() for _ in range(6)]
+outs = [[buffers() for _ in range(20)] for _ in streams]
+torch.cuda.synchronize()
+failed, gate = [], threading.Barrier(len(streams))
+def work(i):
+    try:
+        gate.wait()
+        for out in outs[i]:
+            chain(streams[i], out)
+    except BaseException as e:
+        failed.append(e)
+threads = [threading.Thread(target=work, args=(i,)) for i in range(len(streams))]
+[t.start() for t in threads]
+[t.join() for t in threads]
+torch.cuda.synchronize()
+assert not failed, failed
+first = outs[0][0]
+assert all(torch.equal(a, b) for o in outs for out in o for a, b in zip(first, out))
+assert ((first[5].double().sum(1) - 1).abs() < 1e-4).all() and az.az_tokens_status() == 0
+"""
+    subprocess.run([sys.executable, "-c", code], check=True, cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))), timeout=300)
